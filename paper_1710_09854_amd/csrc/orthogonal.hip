@@ -151,6 +151,13 @@ __device__ __forceinline__ double norm2_of(const Job& J, int64_t t, double (&sum
   return block_sum(s, sums);
 }
 
+// What takes U to X_0, from |U|^2: 0 where U is zero, whatever eps is (with eps = 0 the reciprocal would be infinite and X_0
+// NaN), and NaN where U is not finite.
+__device__ __forceinline__ double inverse_norm(const Job& J, double s2) {
+  if (!(s2 < INFINITY)) return (double)NAN;
+  return s2 > 0.0 ? 1.0 / (sqrt(s2) + J.eps) : 0.0;
+}
+
 // Sums of squares in 64 bits: no overflow or loss whatever the scale of the update. A row is read by 2^k
 // threads, four entries each, several rows at once where it is short. Bound by its bytes: 4096^2 in bfloat16 in 15 us,
 // six 1024 x 4096 with momentum (151 MB) in 39; small matrices by latency (4 to 5 us).
@@ -185,7 +192,7 @@ __global__ void __launch_bounds__(kNormThreads) k_first(Job J) {
     J.norm2[t] = s2;
     if (J.flags) J.flags[t] = !fine ? GSPAR_FLAG_NONFINITE : s2 == 0.0 ? GSPAR_FLAG_ALLZERO : 0u;
   }
-  const double inv = fine ? 1.0 / (sqrt(s2) + J.eps) : (double)NAN;
+  const double inv = inverse_norm(J, s2);
   const int64_t r0 = (int64_t)blockIdx.y * 64, c0 = (int64_t)blockIdx.x * 64;
   char* hi = J.x[0] + t * J.R * J.xrow;
   char* lo = kPairs ? nullptr : J.lo[0] + t * J.R * J.xrow;
@@ -633,7 +640,7 @@ __global__ void __launch_bounds__(kPanelThreads) k_panel(Job J, int from, int to
     if (k == 0 && J.direct && !alone) {
       const double s2 = norm2_of(J, t, sums);
       fine = s2 < INFINITY;
-      inv = fine ? 1.0 / (sqrt(s2) + J.eps) : (double)NAN;
+      inv = inverse_norm(J, s2);
       if (blockIdx.y == 0 && threadIdx.x == 0) {
         J.norm2[t] = s2;
         if (J.flags) J.flags[t] = !fine ? GSPAR_FLAG_NONFINITE : s2 == 0.0 ? GSPAR_FLAG_ALLZERO : 0u;
@@ -751,7 +758,7 @@ __global__ void __launch_bounds__(kPanelThreads) k_panel(Job J, int from, int to
             for (int e = 0; e < 4; ++e) s2 = fma((double)x[b][e], (double)x[b][e], s2);
           s2 = block_sum(s2, sums);
           fine = s2 < INFINITY;
-          inv = fine ? 1.0 / (sqrt(s2) + J.eps) : (double)NAN;
+          inv = inverse_norm(J, s2);
           if (threadIdx.x == 0) {
             J.norm2[t] = s2;
             if (J.flags) J.flags[t] = !fine ? GSPAR_FLAG_NONFINITE : s2 == 0.0 ? GSPAR_FLAG_ALLZERO : 0u;

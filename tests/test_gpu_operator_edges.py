@@ -1,0 +1,75 @@
+"""The feed-forward and update operators where inputs are at the edge of what they promise: updates that are zero,
+momentum past its type's range, views with long pitches, tensors of other streams, autograd.
+
+References are the formulas in 64 bits on the CPU; a tolerance that is not a type's own rounding is derived
+where it stands.
+"""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+NS = (3.4445, -4.7750, 2.0315)
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def gs():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_1710_09854_amd as m
+
+    m.lib()
+    return m
+
+
+def steps64(g, steps=5, coef=NS, eps=1e-7):
+    x = g.detach().cpu().double()
+    x = x / (x.square().sum((-2, -1), keepdim=True).sqrt() + eps)
+    tall = x.shape[-2] > x.shape[-1]
+    if tall:
+        x = x.transpose(-1, -2)
+    for _ in range(steps):
+        a = x @ x.transpose(-1, -2)
+        x = coef[0] * x + (coef[1] * a + coef[2] * a @ a) @ x
+    return x.transpose(-1, -2) if tall else x
+
+
+def off(got, want):
+    got, want = got.detach().cpu().double(), want.detach().cpu().double()
+    assert got.shape == want.shape and bool(torch.isfinite(got).all())
+    return float((got - want).norm() / want.norm().clamp_min(1e-300))
+
+
+def normal(shape, seed, dtype=F32, k=1.0):
+    return torch.from_numpy(k * np.random.default_rng(seed).standard_normal(shape)).to(dtype).cuda()
+
+
+# Every way through the update: tiles read and written by vectors, along and across, and through the last pass; panels
+# that read the caller's rows themselves, several and one; and those that go through the first pass, tall and not.
+PATHS = [(3, 300, 264), (3, 304, 264), (3, 300, 261), (3, 261, 301), (3, 64, 576), (3, 100, 120), (3, 50, 70), (3, 50, 300), (3, 576, 64),
+         (3, 120, 100)]
+
+
+@pytest.mark.parametrize("eps", [0.0, 5e-324, 1e-7])
+@pytest.mark.parametrize("shape", PATHS, ids=str)
+def test_zero_update_stays_zero(gs, shape, eps):
+    """A zero matrix has a zero result whatever is added to its norm (nothing, or a number whose reciprocal is infinite,
+    included), and a step with it only decays the weights."""
+    for dtype in (F32, BF16):
+        g = normal(shape, 1, dtype)
+        g[0], g[2] = 0, 0
+        out = gs.orthogonalize(g, eps=eps)
+        assert out.flags.tolist() == [gs.FLAG_ALLZERO, 0, gs.FLAG_ALLZERO]
+        assert not out.o[0].any() and not out.o[2].any()
+        assert off(out.o[1], steps64(g[1], eps=eps)) <= {F32: 2e-5, BF16: 5e-3}[dtype]
+        w, mom = normal(shape, 2, dtype), torch.zeros(shape, device="cuda")
+        copy = torch.full(shape, 7.0, dtype=F16, device="cuda")
+        decayed = (w.float() * np.float32(0.95)).to(dtype)  # one product in 32 bits, rounded to the type
+        flags = gs.muon_step(w, mom, g, 0.1, weight_decay=0.5, eps=eps, w_copy=copy)
+        assert flags.tolist() == [gs.FLAG_ALLZERO, 0, gs.FLAG_ALLZERO]
+        for k in (0, 2):
+            assert torch.equal(w[k], decayed[k]) and not mom[k].any() and bool(torch.isfinite(copy[k]).all())
+        assert bool(torch.isfinite(w[1]).all()) and not torch.equal(w[1], decayed[1])
