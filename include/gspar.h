@@ -274,8 +274,8 @@ size_t gspar_orthogonalize_workspace_bytes(int64_t batch, int64_t m, int64_t n, 
  * far below the norm to between about 0.7 and 1.2 and leave the singular vectors: out is near U V^T
  * of G = U S V^T.
  *   g and out may have any of the three types each; out may be g itself (the same pointer, type, ld
- *   and stride). coefficients [3] (host). With a 32-bit out the products are as exact as 32-bit
- *   arithmetic; with a 16-bit one they take 11-bit factors around a 22-bit X, below out's own rounding.
+ *   and stride). coefficients [3] (host). With a float32 or float16 out the products are as exact as 32-bit
+ *   arithmetic; with a bfloat16 one they take 11-bit factors around a 22-bit X, below out's own rounding.
  *   flags [batch] uint32 output (may be NULL): GSPAR_FLAG_NONFINITE (G holds Inf or NaN: out is NaN
  *   throughout), GSPAR_FLAG_ALLZERO (out is zero).
  * Errors: GSPAR_ERR_ARG for a NULL or misaligned matrix, an unknown type, batch outside [1, 65535], m

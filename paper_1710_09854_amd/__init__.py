@@ -805,7 +805,8 @@ def orthogonalize(g, steps: int = 5, coefficients=NS_COEFFICIENTS, eps: float = 
                   out_dtype=None, workspace=None, stream=None) -> Orthogonal:
     """Newton-Schulz steps on a matrix or a batch of them (float32, bfloat16 or float16): X = G / (|G|_F
     + eps), then `steps` times X <- c0 X + (c1 A + c2 A^2) X with A = X X^T; o = scale X, in `out`, or a new
-    tensor of out_dtype (g's type when None). A float32 o is as exact as 32-bit products make it."""
+    tensor of out_dtype (g's type when None). A float32 or float16 o is as exact as 32-bit products make it;
+    for a bfloat16 one the products take 11-bit factors, whose errors are below its own rounding."""
     gp, gt, ldg, sg = _matrices(g, "g", _TYPE)
     dev = _on_current_device(g)
     if out is None:

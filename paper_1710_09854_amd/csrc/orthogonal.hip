@@ -8,13 +8,14 @@
 // Precision. Rounding X to 16 bits between steps would lose the directions of small singular values
 // (a matrix of falling strengths comes out 1 to 10 per cent off), because a X lifts them together with
 // their rounding. So X is kept as a sum of two fp16 numbers (22 bits), scaled by 2^12 so that both parts
-// of every entry that matters are normal numbers. With 16-bit results the products take the upper parts
+// of every entry that matters are normal numbers. With bfloat16 results the products take the upper parts
 // alone: their rounding turns a large direction a little, which the next step keeps orthogonal, but does
 // not enter the small ones. The diagonals of A and B are carried in 32 bits beside the products, for near
-// the end a + b + c is 0.7 while its terms are 3.4, 4.8 and 2.0. With 32-bit results each product is
-// upper * upper + upper * lower + lower * upper in 32-bit sums, as exact as 32-bit arithmetic. fp16 and
-// not bf16: after the normalisation nothing exceeds the bound that the host derives from the
-// coefficients, so the range is known and the three more bits are free.
+// the end a + b + c is 0.7 while its terms are 3.4, 4.8 and 2.0. That leaves errors of 3e-4 to 9e-4 (2-norm)
+// where rounding to bfloat16 makes 1.7e-3; rounding to float16 makes 2.1e-4, so float16 results take the other
+// way. With float32 and float16 results each product is upper * upper + upper * lower + lower * upper in 32-bit
+// sums, as exact as 32-bit arithmetic. The parts are fp16 and not bf16: after the normalisation nothing exceeds the
+// bound that the host derives from the coefficients, so the range is known and the three more bits are free.
 #include "dense.h"
 
 #include <algorithm>
@@ -989,6 +990,9 @@ size_t lay_out(Job& J, int64_t batch, int64_t m, int64_t n, bool pairs, char* ws
   return at;
 }
 
+// Whether the products take both parts of X, by the type of the result.
+bool in_pairs(int type) { return type != GSPAR_BF16; }
+
 bool sides_ok(int64_t batch, int64_t m, int64_t n) {
   return batch >= 1 && batch <= 65535 && m >= 1 && n >= 1 && m <= (1 << 20) && n <= (1 << 20);
 }
@@ -1044,7 +1048,7 @@ extern "C" {
 size_t gspar_orthogonalize_workspace_bytes(int64_t batch, int64_t m, int64_t n, int out_type) {
   if (!sides_ok(batch, m, n) || !type_ok(out_type)) return 0;
   Job J;
-  return lay_out(J, batch, m, n, out_type == GSPAR_F32, nullptr);
+  return lay_out(J, batch, m, n, in_pairs(out_type), nullptr);
 }
 
 int gspar_orthogonalize(const void* g, int g_type, int64_t batch, int64_t m, int64_t n, int64_t ldg, int64_t stride_g,
@@ -1055,7 +1059,7 @@ int gspar_orthogonalize(const void* g, int g_type, int64_t batch, int64_t m, int
   J.g = {(void*)g, ldg, stride_g, g_type};
   J.out = {out, ldo, stride_o, out_type};
   if (!tensor_ok(J.g, batch, m, n) || !tensor_ok(J.out, batch, m, n)) return GSPAR_ERR_ARG;
-  const bool pairs = out_type == GSPAR_F32;
+  const bool pairs = in_pairs(out_type);
   if (const int rc = common(J, batch, m, n, pairs, steps, coefficients, eps, ws, ws_bytes)) return rc;
   J.rate = (float)scale;
   J.flags = flags;
@@ -1080,7 +1084,7 @@ int gspar_muon_step(void* w, int w_type, int64_t ldw, int64_t stride_w, void* mo
     J.half = {w_copy, ldc, stride_c, copy_type};
     if (!tensor_ok(J.half, batch, m, n)) return GSPAR_ERR_ARG;
   }
-  const bool pairs = w_type == GSPAR_F32;
+  const bool pairs = in_pairs(w_type);
   if (const int rc = common(J, batch, m, n, pairs, steps, coefficients, eps, ws, ws_bytes)) return rc;
   J.beta = (float)beta;
   J.nesterov = nesterov != 0;

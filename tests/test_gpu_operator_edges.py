@@ -73,3 +73,25 @@ def test_zero_update_stays_zero(gs, shape, eps):
         for k in (0, 2):
             assert torch.equal(w[k], decayed[k]) and not mom[k].any() and bool(torch.isfinite(copy[k]).all())
         assert bool(torch.isfinite(w[1]).all()) and not torch.equal(w[1], decayed[1])
+
+
+@pytest.mark.parametrize("kind", ["normal", "low"])
+@pytest.mark.parametrize("shape", [(64, 576), (128, 1024), (1024, 128), (100, 120), (300, 520), (777, 333), (512, 2048), (260, 4001)], ids=str)
+def test_float16_results_are_rounded_once(gs, shape, kind):
+    """A float16 result is off by its own rounding. Tolerance, on 2-norms: what rounding the formula's result costs, which
+    over 12,000 elements and more is the same for a result within 2e-5 of it to a few per cent (a tenth is
+    allowed), and the 2e-5 to which 32-bit results of rank 32 and more are held."""
+    g = normal(shape, 3)
+    if kind == "low":
+        r = min(shape) // 8
+        g = normal((shape[0], r), 4) @ normal((r, shape[1]), 5) / math.sqrt(r) + 0.1 * g
+    for t in (F16, F32):
+        x = g.to(t)
+        want = steps64(x)
+        most = 1.1 * off(want.half(), want) + 2e-5
+        assert off(gs.orthogonalize(x, out_dtype=F16).o, want) <= most
+    # the same for weights, where all of them is the update
+    w, mom = torch.zeros(shape, dtype=F16, device="cuda"), torch.zeros(shape, device="cuda")
+    gs.muon_step(w, mom, g, 1.0, beta=0.5, nesterov=False)
+    want = -steps64(g)
+    assert off(w, want) <= 1.1 * off(want.half(), want) + 2e-5
