@@ -922,10 +922,10 @@ int run_job(Job& J, hipStream_t s) {
       typedef decltype(tile) C;
       const int tr = (int)ceil_div(J.R, C::BM), tc = (int)ceil_div(J.C, C::BN);
       const dim3 grid(tr * tc, batch), block(C::kThreads);
-      // A step lifts the rounding of its X by a at most. The last one's, 2^-12 a for the usual a of 3.4, is below what
+      // A step lifts the rounding of its X by |a| at most. The last one's, 2^-12 |a| for the usual a of 3.4, is below what
       // the products' roundings leave: its X goes without lower parts (6 x 1024 x 4096, the last product: 115 -> 110 us).
-      // A larger a keeps them.
-      const bool light = J.a <= 4.f, whole = !light || k == 0 || k + 1 < J.steps, keep = !light || k + 2 != J.steps;
+      // A larger |a| keeps them. (Pairs have both parts in one place, and keep them.)
+      const bool light = std::fabs(J.a) <= 4.f, whole = !light || k == 0 || k + 1 < J.steps, keep = !light || k + 2 != J.steps;
       if (k + 1 < J.steps || !vec) hipLaunchKernelGGL((k_apply<C, false, false>), grid, block, 0, s, J, w, tr, tc, whole, keep);
       else if (!J.tall) hipLaunchKernelGGL((k_apply<C, true, false>), grid, block, 0, s, J, w, tr, tc, whole, keep);
       else hipLaunchKernelGGL((k_apply<C, true, true>), grid, block, 0, s, J, w, tc, tr, whole, keep);

@@ -95,3 +95,22 @@ def test_float16_results_are_rounded_once(gs, shape, kind):
     gs.muon_step(w, mom, g, 1.0, beta=0.5, nesterov=False)
     want = -steps64(g)
     assert off(w, want) <= 1.1 * off(want.half(), want) + 2e-5
+
+
+@pytest.mark.parametrize("shape", [(200, 300), (304, 200), (264, 520), (260, 261)], ids=str)
+def test_coefficients_of_the_other_sign(gs, shape):
+    """With all coefficients negated a step gives -X in place of X, through the same roundings: what is kept in fewer bits
+    goes by a coefficient's size. Seen in the 32-bit copy of bfloat16 weights, whose products take the upper parts.
+
+    Tolerance: the matrix cores' 32-bit sums may differ in their last bits when one side is negated (2 in 1000 do). Were all
+    off by 2^-23, one of 2^13 roundings to 11 bits would turn by a whole place, 2^-10: 2^-10 * 2^-6.5 = 1.1e-5 of A, of B
+    and of the upper parts in each of three steps, 3.3e-5 in all. A last X without its lower parts shows as 8e-5 or more
+    with the first set."""
+    for coef in ((4.5, -8.0, 3.0), NS):
+        g, got = normal(shape, 6), []
+        for sign in (1, -1):
+            w, copy = torch.zeros(shape, dtype=BF16, device="cuda"), torch.zeros(shape, device="cuda")
+            gs.muon_step(w, torch.zeros(shape, device="cuda"), g, sign, nesterov=False, steps=3,
+                         coefficients=tuple(sign * c for c in coef), w_copy=copy)
+            got.append(copy)
+        assert off(got[1], got[0]) <= 4e-5, coef
