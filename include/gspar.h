@@ -294,8 +294,9 @@ int gspar_orthogonalize(const void* g, int g_type, int64_t batch, int64_t m, int
  *   w, momentum and g may have any of the three types each; arithmetic between them is in 32 bits, and
  *   the products are taken as gspar_orthogonalize takes them for an out of w's type.
  *   w_copy (may be NULL): a second copy of the new weights in another type.
- *   flags as above. Where U holds Inf or NaN, w, momentum and w_copy of that matrix are left as they
- *   were: a step that overflowed is skipped.
+ *   flags as above. Where U holds Inf or NaN, or the new momentum a number that its type cannot hold, the
+ *   flag is GSPAR_FLAG_NONFINITE and w, momentum and w_copy of that matrix are left as they were: a step that
+ *   overflowed is skipped. (A new weight past its type's range is stored as that type's infinity.)
  * Errors: as above, and GSPAR_ERR_ARG for a non-finite lr, weight_decay or scale or a negative or
  * non-finite beta. */
 int gspar_muon_step(void* w, int w_type, int64_t ldw, int64_t stride_w, void* momentum, int momentum_type,

@@ -835,7 +835,7 @@ def muon_step(w, momentum, grad, lr: float, beta: float = 0.95, nesterov: bool =
     beta momentum (nesterov) or momentum, w <- (1 - lr weight_decay) w - lr scale O(U) with O the orthogonalisation
     of ``orthogonalize``. w_copy receives the new weights in a second type (w in float32 and the copy that
     the next forward pass multiplies with, say). Returns the flags (int32, one per matrix); a matrix whose U is not
-    finite is left as it was."""
+    finite, or whose momentum its type cannot hold, is left as it was."""
     wp, wt, ldw, sw = _matrices(w, "w", _TYPE)
     dev = _on_current_device(w)
     mp, mt, ldm, sm = _matrices(momentum, "momentum", _TYPE, w)

@@ -114,15 +114,22 @@ struct Job {
 // ------------------------------------------------------------------------------------------
 constexpr int kNormThreads = 256;
 
-// Four entries of U from (i, j) on, of which n are there; the new momentum in mnew.
+// From this magnitude on a number is an infinity in a tensor of the type: half a place past its largest number.
+__device__ __forceinline__ float past_range(int type) {
+  return type == GSPAR_F16 ? 65520.f : type == GSPAR_BF16 ? 0x1.FFp127f : INFINITY;
+}
+
+// Four entries of U from (i, j) on, of which n are there; the new momentum in mnew. A momentum that its type cannot hold
+// makes U infinite, and so its matrix's step one that is skipped.
 __device__ __forceinline__ f32x4 update_at(const Job& J, int64_t t, int64_t i, int64_t j, int64_t n, f32x4& mnew) {
   f32x4 g = load4(J.g.p, t * J.g.stride + i * J.g.ld + j, J.g.type, n);
   if (!J.mom.p) return g;
   mnew = load4(J.mom.p, t * J.mom.stride + i * J.mom.ld + j, J.mom.type, n);
+  const float past = past_range(J.mom.type);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     mnew[e] = fmaf(J.beta, mnew[e], g[e]);
-    g[e] = J.nesterov ? fmaf(J.beta, mnew[e], g[e]) : mnew[e];
+    g[e] = !(fabsf(mnew[e]) < past) ? INFINITY : J.nesterov ? fmaf(J.beta, mnew[e], g[e]) : mnew[e];
   }
   return g;
 }
@@ -743,12 +750,13 @@ __global__ void __launch_bounds__(kPanelThreads) k_panel(Job J, int from, int to
         load_fours<RB>(J, J.g, t, lr, c, x);
         if (J.mom.p) {
           load_fours<RB>(J, J.mom, t, lr, c, m);
+          const float past = past_range(J.mom.type);
 #pragma unroll
           for (int b = 0; b < RB; ++b)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               m[b][e] = fmaf(J.beta, m[b][e], x[b][e]);
-              x[b][e] = J.nesterov ? fmaf(J.beta, m[b][e], x[b][e]) : m[b][e];
+              x[b][e] = !(fabsf(m[b][e]) < past) ? INFINITY : J.nesterov ? fmaf(J.beta, m[b][e], x[b][e]) : m[b][e];
             }
         }
         if (alone) {

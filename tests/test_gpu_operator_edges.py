@@ -114,3 +114,27 @@ def test_coefficients_of_the_other_sign(gs, shape):
                          coefficients=tuple(sign * c for c in coef), w_copy=copy)
             got.append(copy)
         assert off(got[1], got[0]) <= 4e-5, coef
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("shape", PATHS, ids=str)
+def test_momentum_past_its_range(gs, shape, nesterov):
+    """A new momentum that its type cannot hold skips the matrix's step like any overflow, and a later one that it can
+    hold takes it."""
+    # float16: 0.95 * 6e4 + 1e4 = 67,000, past 65,504. bfloat16: its largest number is 255/256 * 2^128, to which 1e36
+    # adds more than half of the last place, 2^119 = 6.6e35.
+    for mt, beta, m0, g0 in ((F16, 0.95, 6e4, 1e4), (BF16, 1.0, float(torch.finfo(BF16).max), 1e36)):
+        if mt == BF16 and nesterov:
+            continue  # U itself is past 32 bits then
+        w, mom, g = normal(shape, 7), normal(shape, 8, mt), normal(shape, 9)
+        mom[1, 3, 5], g[1, 3, 5] = m0, g0
+        w0, mom0 = w.clone(), mom.clone()
+        copy = torch.full(shape, 3.0, dtype=BF16, device="cuda")
+        flags = gs.muon_step(w, mom, g, 0.1, beta=beta, nesterov=nesterov, w_copy=copy)
+        assert flags.tolist() == [0, gs.FLAG_NONFINITE, 0]
+        assert torch.equal(w[1], w0[1]) and torch.equal(mom[1], mom0[1]) and bool((copy[1] == 3.0).all())
+        for k in (0, 2):
+            assert not torch.equal(w[k], w0[k]) and not torch.equal(mom[k], mom0[k])
+        g[1, 3, 5] = 0.0
+        assert not gs.muon_step(w, mom, g, 0.1, beta=beta, nesterov=nesterov, w_copy=copy).any()
+        assert bool(torch.isfinite(mom).all()) and not torch.equal(w[1], w0[1]) and torch.equal(copy, w.bfloat16())
