@@ -311,7 +311,8 @@ int gspar_muon_step(void* w, int w_type, int64_t ldw, int64_t stride_w, void* mo
 size_t gspar_gated_ff_saved_bytes(int64_t tokens, int64_t d_hidden);
 
 /* Workspace of a forward (backward = 0) or backward pass; `aligned`: every row of x, w_gate and w_up
- * starts on a 16-byte boundary (then none of them is copied). */
+ * starts on a 16-byte boundary, and none of their leading dimensions is over 4,000,000 (of one row it is not looked
+ * at): then none of them is copied. 0 is always enough. */
 size_t gspar_gated_ff_workspace_bytes(int64_t tokens, int64_t d_in, int64_t d_hidden, int aligned, int backward);
 
 /* Gated feed-forward block, h = act(x w_gate^T) * (x w_up^T): x [tokens][d_in], w_gate and w_up

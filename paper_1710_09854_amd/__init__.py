@@ -889,7 +889,7 @@ def _ff_operands(x, w_gate, w_up, act):
         raise ValueError(f"the weights are on {w_gate.device}, not on {x.device}")
     if act not in _ACT:
         raise ValueError(f"unknown activation {act!r}")
-    aligned = 0 if (xp | gp | up) & 15 or (ldx | ldg | ldu | d) & 7 else 1
+    aligned = 0 if (xp | gp | up) & 15 or (ldx | ldg | ldu | d) & 7 or max(ldx, ldg, ldu) > 4_000_000 else 1
     return xp, ldx, gp, ldg, up, ldu, t, T, d, f, _ACT[act], aligned, dev
 
 

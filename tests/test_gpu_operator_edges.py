@@ -138,3 +138,24 @@ def test_momentum_past_its_range(gs, shape, nesterov):
         g[1, 3, 5] = 0.0
         assert not gs.muon_step(w, mom, g, 0.1, beta=beta, nesterov=nesterov, w_copy=copy).any()
         assert bool(torch.isfinite(mom).all()) and not torch.equal(w[1], w0[1]) and torch.equal(copy, w.bfloat16())
+
+
+def test_long_pitches(gs):
+    """Rows on 16-byte boundaries further apart than a tile's reads of them reach: a workspace of its own is large enough
+    for the copies that such operands take."""
+    T, d, f, far = 33, 64, 40, 4_000_008
+    x, wg, wu, dh = normal((T, d), 10, BF16), normal((f, d), 11, BF16, 0.125), normal((f, d), 12, BF16, 0.125), normal((T, f), 13, BF16)
+    want = gs.gated_ff(x, wg, wu, save=True)
+    ref = gs.gated_ff_backward(dh, x, wg, wu, want.saved)
+
+    def spread(t):
+        big = torch.zeros(((t.shape[0] - 1) * far + t.shape[1],), dtype=t.dtype, device="cuda")
+        view = big.as_strided(t.shape, (far, 1))
+        view.copy_(t)
+        return view
+
+    for a, b in ((spread(x), wg), (x, spread(wg))):
+        y = gs.gated_ff(a, b, wu, save=True, workspace=gs.Workspace())
+        assert torch.equal(y.h, want.h) and torch.equal(y.saved, want.saved)
+        got = gs.gated_ff_backward(dh, a, b, wu, y.saved, workspace=gs.Workspace())
+        assert all(torch.equal(p, q) for p, q in zip((got.dx, got.dw_gate, got.dw_up), (ref.dx, ref.dw_gate, ref.dw_up)))
