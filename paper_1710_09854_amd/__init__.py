@@ -801,14 +801,35 @@ class Orthogonal:
     flags: torch.Tensor
 
 
+class _Underived(torch.autograd.Function):
+    """An orthogonalisation in the graph, for its backward pass to raise an error and not to leave a part out."""
+
+    @staticmethod
+    def forward(ctx, g, call):
+        r = call()
+        ctx.mark_non_differentiable(r.flags)
+        return r.o, r.flags
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("orthogonalize has no derivative: call it on g.detach() or under torch.no_grad()")
+
+
 def orthogonalize(g, steps: int = 5, coefficients=NS_COEFFICIENTS, eps: float = 1e-7, scale: float = 1.0, out=None,
                   out_dtype=None, workspace=None, stream=None) -> Orthogonal:
     """Newton-Schulz steps on a matrix or a batch of them (float32, bfloat16 or float16): X = G / (|G|_F
     + eps), then `steps` times X <- c0 X + (c1 A + c2 A^2) X with A = X X^T; o = scale X, in `out`, or a new
     tensor of out_dtype (g's type when None). A float32 or float16 o is as exact as 32-bit products make it;
-    for a bfloat16 one the products take 11-bit factors, whose errors are below its own rounding."""
+    for a bfloat16 one the products take 11-bit factors, whose errors are below its own rounding. It has no derivative:
+    a backward pass that arrives at an o of a g that requires a gradient raises an error."""
     gp, gt, ldg, sg = _matrices(g, "g", _TYPE)
     dev = _on_current_device(g)
+    if g.requires_grad and torch.is_grad_enabled():
+        if out is not None:
+            raise RuntimeError("orthogonalize(out=...) is no part of autograd, and g requires a gradient")
+        with torch.cuda.stream(stream):
+            return Orthogonal(*_Underived.apply(g, lambda: orthogonalize(g, steps, coefficients, eps, scale, None, out_dtype,
+                                                                         workspace)))
     if out is None:
         out = torch.empty(g.shape, dtype=g.dtype if out_dtype is None else out_dtype, device=g.device)
         _made_for(stream, out)
@@ -893,10 +914,37 @@ def _ff_operands(x, w_gate, w_up, act):
     return xp, ldx, gp, ldg, up, ldu, t, T, d, f, _ACT[act], aligned, dev
 
 
+class _GatedFFNode(torch.autograd.Function):
+    """The block as a node of autograd's graph."""
+
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, act, workspace):
+        y = gated_ff(x, w_gate, w_up, act, True, None, workspace)
+        ctx.save_for_backward(x, w_gate, w_up, y.saved)
+        ctx.mark_non_differentiable(y.saved)
+        ctx.act = act
+        return y.h, y.saved
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dh, _):
+        # what a loss hands over may be expanded or transposed
+        d = gated_ff_backward(dh.contiguous(), *ctx.saved_tensors, ctx.act, ctx.needs_input_grad[:3])
+        return d.dx, d.dw_gate, d.dw_up, None, None
+
+
 def gated_ff(x, w_gate, w_up, act: str = "silu", save: bool = False, out=None, workspace=None, stream=None) -> GatedFF:
     """h = act(x w_gate^T) * (x w_up^T) for x [tokens, d_in] and weights [d_hidden, d_in], all bfloat16 or
-    float16 (act: "silu", "gelu" or "gelu_tanh"); save=True also keeps what ``gated_ff_backward`` needs."""
+    float16 (act: "silu", "gelu" or "gelu_tanh"); save=True also keeps what ``gated_ff_backward`` needs. In grad mode,
+    where an input requires a gradient, h is a node of the graph whose backward pass is ``gated_ff_backward`` (once: it has
+    no second derivative), with a default workspace, on the forward pass's stream; `out` is refused then."""
     xp, ldx, gp, ldg, up, ldu, t, T, d, f, a, aligned, dev = _ff_operands(x, w_gate, w_up, act)
+    if (x.requires_grad or w_gate.requires_grad or w_up.requires_grad) and torch.is_grad_enabled():
+        if out is not None:
+            raise RuntimeError("gated_ff(out=...) is no part of autograd, and an input requires a gradient")
+        with torch.cuda.stream(stream):
+            h, saved = _GatedFFNode.apply(x, w_gate, w_up, act, workspace)
+        return GatedFF(h, saved if save else None)
     if out is None:
         out = torch.empty((T, f), dtype=x.dtype, device=x.device)
         _made_for(stream, out)

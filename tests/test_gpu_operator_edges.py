@@ -159,3 +159,88 @@ def test_long_pitches(gs):
         assert torch.equal(y.h, want.h) and torch.equal(y.saved, want.saved)
         got = gs.gated_ff_backward(dh, a, b, wu, y.saved, workspace=gs.Workspace())
         assert all(torch.equal(p, q) for p, q in zip((got.dx, got.dw_gate, got.dw_up), (ref.dx, ref.dw_gate, ref.dw_up)))
+
+
+def ff_inputs(T, d, f, dtype, seed):
+    return (normal((T, d), seed, dtype), normal((f, d), seed + 1, dtype, 1.5 / math.sqrt(d)),
+            normal((f, d), seed + 2, dtype, 1 / math.sqrt(d)), normal((T, f), seed + 3, dtype, 0.1))
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("T", [3, 70])
+def test_autograd_reaches_the_block(gs, T, act):
+    """Under grad mode the block is a node of the graph: the gradients are those of gated_ff_backward, bit for bit."""
+    x, wg, wu, dh = ff_inputs(T, 72, 100, BF16, 20)
+    y = gs.gated_ff(x, wg, wu, act, save=True)
+    ref = gs.gated_ff_backward(dh, x, wg, wu, y.saved, act)
+    ref = (ref.dx, ref.dw_gate, ref.dw_up)
+    assert not y.h.requires_grad
+    for want in ((True, True, True), (True, False, False), (False, True, False), (False, False, True)):
+        for save in (False, True):
+            t = [a.clone().requires_grad_(w) for a, w in zip((x, wg, wu), want)]
+            z = gs.gated_ff(*t, act, save=save)
+            assert torch.equal(z.h, y.h) and z.h.requires_grad
+            assert (z.saved is not None) == save
+            if save:  # rows' padding in it is not written: what counts is what comes of it
+                assert not z.saved.requires_grad
+                d = gs.gated_ff_backward(dh, x, wg, wu, z.saved, act)
+                assert all(torch.equal(a, r) for a, r in zip((d.dx, d.dw_gate, d.dw_up), ref))
+            z.h.backward(dh)
+            for a, w, r in zip(t, want, ref):
+                assert torch.equal(a.grad, r) if w else a.grad is None
+    # what a loss's backward pass hands over may be an expanded number or a transposed matrix
+    ones = gs.gated_ff_backward(torch.ones_like(dh), x, wg, wu, y.saved, act)
+    t = x.clone().requires_grad_()
+    gs.gated_ff(t, wg, wu, act).h.sum().backward()
+    assert torch.equal(t.grad, ones.dx)
+    t = x.clone().requires_grad_()
+    (gs.gated_ff(t, wg, wu, act).h.t() * dh.t()).sum().backward()
+    assert torch.equal(t.grad, ref[0])
+
+
+def test_autograd_of_a_residual_layer(gs):
+    """x + W h: the part that comes through the block is in x's gradient (to the two roundings of their sum)."""
+    x, wg, wu, _ = ff_inputs(40, 64, 96, BF16, 30)
+    down, dy = normal((96, 64), 34, BF16, 0.1), normal((40, 64), 35, BF16)
+    leaf = [t.clone().requires_grad_() for t in (x, wg, wu)]
+    (leaf[0] + gs.gated_ff(*leaf).h @ down).backward(dy)
+    y = gs.gated_ff(x, wg, wu, save=True)
+    d = gs.gated_ff_backward(dy @ down.t(), x, wg, wu, y.saved)
+    assert off(leaf[0].grad, dy.double() + d.dx.double()) <= 2.0 ** -8
+    assert torch.equal(leaf[1].grad, d.dw_gate) and torch.equal(leaf[2].grad, d.dw_up)
+
+
+def test_autograd_where_there_is_no_graph(gs):
+    x, wg, wu, dh = ff_inputs(8, 16, 24, F16, 40)
+    want = gs.gated_ff(x, wg, wu).h
+    out = torch.empty_like(want)
+    p = wg.clone().requires_grad_()
+    with torch.no_grad():
+        assert not gs.gated_ff(x, p, wu).h.requires_grad
+        assert torch.equal(gs.gated_ff(x, p, wu, out=out).h, want)
+    with torch.inference_mode():
+        assert torch.equal(gs.gated_ff(x, p, wu, out=out).h, want) and torch.equal(gs.gated_ff(x, p, wu, out=torch.empty_like(want)).h, want)
+    with pytest.raises(RuntimeError):  # as torch's own functions
+        gs.gated_ff(x, p, wu, out=out)
+    # the formulas' second derivatives are not there, and nothing passes for them
+    t = x.clone().requires_grad_()
+    g, = torch.autograd.grad(gs.gated_ff(t, p, wu).h, t, dh, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+    # a product by hand, as before
+    y = gs.gated_ff(x, p.detach(), wu, save=True)
+    assert not gs.gated_ff_backward(dh, x, p, wu, y.saved).dx.requires_grad
+
+
+def test_orthogonalize_has_no_derivative(gs):
+    """It is no part of what is differentiated; a backward pass that arrives there is told so."""
+    g = normal((20, 30), 50).requires_grad_()
+    want = gs.orthogonalize(g.detach())
+    o = gs.orthogonalize(g)
+    assert torch.equal(o.o, want.o) and torch.equal(o.flags, want.flags) and o.o.requires_grad and not o.flags.requires_grad
+    with pytest.raises(RuntimeError, match="derivative"):
+        o.o.sum().backward()
+    with torch.no_grad():
+        assert not gs.orthogonalize(g).o.requires_grad
+    with pytest.raises(RuntimeError):
+        gs.orthogonalize(g, out=torch.empty_like(want.o))
