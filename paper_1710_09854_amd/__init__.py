@@ -774,6 +774,14 @@ def _made_for(stream, *tensors):
                 t.record_stream(stream)
 
 
+def _written(*tensors):
+    """Counts the write of a call into the caller's tensors, which autograd cannot see: a backward pass that still needs
+    their old values raises an error."""
+    for t in tensors:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
+
+
 def _on_current_device(t) -> int:
     """The device's index; a call enqueues its kernels on the current device."""
     i = t.get_device()
@@ -846,6 +854,7 @@ def orthogonalize(g, steps: int = 5, coefficients=NS_COEFFICIENTS, eps: float = 
     rc = L.gspar_orthogonalize(gp, gt, batch, m, n, ldg, sg, int(steps), c, float(eps), float(scale), op, ot, ldo, so,
                                fl.data_ptr(), buf, nb, raw)
     _check(rc, "gspar_orthogonalize")
+    _written(out)
     return Orthogonal(out, fl)
 
 
@@ -873,6 +882,7 @@ def muon_step(w, momentum, grad, lr: float, beta: float = 0.95, nesterov: bool =
                            1 if nesterov else 0, float(weight_decay), float(scale), int(steps), c, float(eps), cp, ct, ldc, sc,
                            fl.data_ptr(), buf, nb, raw)
     _check(rc, "gspar_muon_step")
+    _written(w, momentum, w_copy)
     return fl
 
 
@@ -961,6 +971,7 @@ def gated_ff(x, w_gate, w_up, act: str = "silu", save: bool = False, out=None, w
     rc = L.gspar_gated_ff_forward(xp, ldx, gp, ldg, up, ldu, t, T, d, f, a, hp, ldh, sp, buf, nb, raw)
     if rc != OK:
         _check(rc, "gspar_gated_ff_forward")
+    _written(out)
     return GatedFF(out, saved)
 
 

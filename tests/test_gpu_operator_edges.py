@@ -244,3 +244,28 @@ def test_orthogonalize_has_no_derivative(gs):
         assert not gs.orthogonalize(g).o.requires_grad
     with pytest.raises(RuntimeError):
         gs.orthogonalize(g, out=torch.empty_like(want.o))
+
+
+def test_writes_are_seen_by_autograd(gs):
+    """What a call writes in place counts as modified: a backward pass that still needs the old values says so."""
+    w, mom, copy = normal((40, 64), 60), normal((40, 64), 61), torch.zeros((40, 64), dtype=BF16, device="cuda")
+    g = normal((40, 64), 62)
+    before = [t._version for t in (w, mom, copy, g)]
+    x = normal((8, 64), 63).requires_grad_()
+    loss = (x @ w.t()).sum()  # keeps w for x's gradient
+    gs.muon_step(w, mom, g, 0.1, w_copy=copy)
+    assert all(t._version > v for t, v in zip((w, mom, copy), before)) and g._version == before[3]
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    v = w._version
+    gs.orthogonalize(g, out=w)
+    assert w._version > v
+    x, wg, wu, _ = ff_inputs(8, 16, 24, F16, 64)
+    h = torch.zeros((8, 24), dtype=F16, device="cuda")
+    v = h._version
+    gs.gated_ff(x, wg, wu, out=h)
+    assert h._version > v
+    with torch.inference_mode():  # tensors that keep no count
+        t = torch.zeros((40, 64), device="cuda")
+        gs.muon_step(t, torch.zeros_like(t), g, 0.1)
+        assert bool(t.any())
