@@ -766,8 +766,19 @@ def _matrices(t, what, types, like=None):
     return t.data_ptr(), _TYPE[t.dtype], ld, stride
 
 
-def _made_for(stream, *tensors):
-    """Tensors made here on the current stream and written on another one."""
+def _empty(shape, dtype, device, stream):
+    """A result of a call. Where the call goes to a stream of its own, the memory is that stream's: from the current one's
+    pool it could be memory that earlier work there has yet to write. It is the current stream's to read as well."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _lend(stream, *tensors):
+    """Keeps the memory of tensors that a call on another stream reads or writes until that stream is done with it."""
     if stream is not None:
         for t in tensors:
             if t is not None:
@@ -782,11 +793,13 @@ def _written(*tensors):
             torch.autograd.graph.increment_version(t)
 
 
-def _on_current_device(t) -> int:
-    """The device's index; a call enqueues its kernels on the current device."""
+def _on_current_device(t, stream=None) -> int:
+    """The device's index; a call enqueues its kernels on the current device, whose the stream has to be too."""
     i = t.get_device()
     if i != torch._C._cuda_getDevice():
         raise ValueError(f"the tensors are on {t.device}, and the current device is cuda:{torch.cuda.current_device()}")
+    if stream is not None and stream.device_index != i:
+        raise ValueError(f"the tensors are on {t.device}, and the stream on cuda:{stream.device_index}")
     return i
 
 
@@ -831,23 +844,21 @@ def orthogonalize(g, steps: int = 5, coefficients=NS_COEFFICIENTS, eps: float = 
     for a bfloat16 one the products take 11-bit factors, whose errors are below its own rounding. It has no derivative:
     a backward pass that arrives at an o of a g that requires a gradient raises an error."""
     gp, gt, ldg, sg = _matrices(g, "g", _TYPE)
-    dev = _on_current_device(g)
+    dev = _on_current_device(g, stream)
     if g.requires_grad and torch.is_grad_enabled():
         if out is not None:
             raise RuntimeError("orthogonalize(out=...) is no part of autograd, and g requires a gradient")
-        with torch.cuda.stream(stream):
-            return Orthogonal(*_Underived.apply(g, lambda: orthogonalize(g, steps, coefficients, eps, scale, None, out_dtype,
-                                                                         workspace)))
+        return Orthogonal(*_Underived.apply(g, lambda: orthogonalize(g, steps, coefficients, eps, scale, None, out_dtype,
+                                                                     workspace, stream)))
     if out is None:
-        out = torch.empty(g.shape, dtype=g.dtype if out_dtype is None else out_dtype, device=g.device)
-        _made_for(stream, out)
+        out = _empty(g.shape, g.dtype if out_dtype is None else out_dtype, g.device, stream)
     elif out_dtype is not None and out.dtype != out_dtype:
         raise ValueError("out is not of out_dtype")
     op, ot, ldo, so = _matrices(out, "out", _TYPE, g)
     m, n = g.shape[-2:]
     batch = g.shape[0] if g.dim() == 3 else 1
-    fl = torch.empty(batch, dtype=torch.int32, device=g.device)
-    _made_for(stream, fl)
+    fl = _empty(batch, torch.int32, g.device, stream)
+    _lend(stream, g, out)
     L = lib()
     buf, nb, raw = _place(workspace, dev, L.gspar_orthogonalize_workspace_bytes(batch, m, n, ot), stream)
     c = (ctypes.c_double * 3)(*coefficients)
@@ -867,14 +878,14 @@ def muon_step(w, momentum, grad, lr: float, beta: float = 0.95, nesterov: bool =
     the next forward pass multiplies with, say). Returns the flags (int32, one per matrix); a matrix whose U is not
     finite, or whose momentum its type cannot hold, is left as it was."""
     wp, wt, ldw, sw = _matrices(w, "w", _TYPE)
-    dev = _on_current_device(w)
+    dev = _on_current_device(w, stream)
     mp, mt, ldm, sm = _matrices(momentum, "momentum", _TYPE, w)
     gp, gt, ldg, sg = _matrices(grad, "grad", _TYPE, w)
     cp, ct, ldc, sc = (None, 0, 0, 0) if w_copy is None else _matrices(w_copy, "w_copy", _TYPE, w)
     m, n = w.shape[-2:]
     batch = w.shape[0] if w.dim() == 3 else 1
-    fl = torch.empty(batch, dtype=torch.int32, device=w.device)
-    _made_for(stream, fl)
+    fl = _empty(batch, torch.int32, w.device, stream)
+    _lend(stream, w, momentum, grad, w_copy)
     L = lib()
     buf, nb, raw = _place(workspace, dev, L.gspar_orthogonalize_workspace_bytes(batch, m, n, wt), stream)
     c = (ctypes.c_double * 3)(*coefficients)
@@ -903,7 +914,7 @@ class GatedFFGrads:
 _FF_TYPES = (torch.bfloat16, torch.float16)
 
 
-def _ff_operands(x, w_gate, w_up, act):
+def _ff_operands(x, w_gate, w_up, act, stream):
     xp, t, ldx, _ = _matrices(x, "x", _FF_TYPES)
     gp, gt, ldg, _ = _matrices(w_gate, "w_gate", _FF_TYPES)
     up, ut, ldu, _ = _matrices(w_up, "w_up", _FF_TYPES, w_gate)
@@ -915,7 +926,7 @@ def _ff_operands(x, w_gate, w_up, act):
     f = w_gate.shape[0]
     if d != w_gate.shape[1]:
         raise ValueError(f"x has {d} columns and the weights {w_gate.shape[1]}")
-    dev = _on_current_device(x)
+    dev = _on_current_device(x, stream)
     if w_gate.get_device() != dev:
         raise ValueError(f"the weights are on {w_gate.device}, not on {x.device}")
     if act not in _ACT:
@@ -948,25 +959,27 @@ def gated_ff(x, w_gate, w_up, act: str = "silu", save: bool = False, out=None, w
     float16 (act: "silu", "gelu" or "gelu_tanh"); save=True also keeps what ``gated_ff_backward`` needs. In grad mode,
     where an input requires a gradient, h is a node of the graph whose backward pass is ``gated_ff_backward`` (once: it has
     no second derivative), with a default workspace, on the forward pass's stream; `out` is refused then."""
-    xp, ldx, gp, ldg, up, ldu, t, T, d, f, a, aligned, dev = _ff_operands(x, w_gate, w_up, act)
+    xp, ldx, gp, ldg, up, ldu, t, T, d, f, a, aligned, dev = _ff_operands(x, w_gate, w_up, act, stream)
     if (x.requires_grad or w_gate.requires_grad or w_up.requires_grad) and torch.is_grad_enabled():
         if out is not None:
             raise RuntimeError("gated_ff(out=...) is no part of autograd, and an input requires a gradient")
+        here = torch.cuda.current_stream()
+        _lend(stream, x, w_gate, w_up)
         with torch.cuda.stream(stream):
             h, saved = _GatedFFNode.apply(x, w_gate, w_up, act, workspace)
+        _lend(None if stream is None else here, h, saved)
         return GatedFF(h, saved if save else None)
     if out is None:
-        out = torch.empty((T, f), dtype=x.dtype, device=x.device)
-        _made_for(stream, out)
+        out = _empty((T, f), x.dtype, x.device, stream)
     elif out.dtype != x.dtype or out.shape != (T, f) or out.get_device() != dev:
         raise ValueError(f"out must be {x.dtype} of shape {(T, f)} on {x.device}")
     hp, _, ldh, _ = _matrices(out, "out", _FF_TYPES)
     L = lib()
     saved, sp = None, None
     if save:
-        saved = torch.empty(L.gspar_gated_ff_saved_bytes(T, f), dtype=torch.uint8, device=x.device)
-        _made_for(stream, saved)
+        saved = _empty(L.gspar_gated_ff_saved_bytes(T, f), torch.uint8, x.device, stream)
         sp = saved.data_ptr()
+    _lend(stream, x, w_gate, w_up, out)
     buf, nb, raw = _place(workspace, dev, L.gspar_gated_ff_workspace_bytes(T, d, f, aligned, 0), stream)
     rc = L.gspar_gated_ff_forward(xp, ldx, gp, ldg, up, ldu, t, T, d, f, a, hp, ldh, sp, buf, nb, raw)
     if rc != OK:
@@ -978,7 +991,7 @@ def gated_ff(x, w_gate, w_up, act: str = "silu", save: bool = False, out=None, w
 def gated_ff_backward(dh, x, w_gate, w_up, saved, act: str = "silu", want=(True, True, True), workspace=None,
                       stream=None) -> GatedFFGrads:
     """The gradients of x, w_gate and w_up (None where `want` is false) from dh and what the forward pass kept."""
-    xp, ldx, gp, ldg, up, ldu, t, T, d, f, a, aligned, index = _ff_operands(x, w_gate, w_up, act)
+    xp, ldx, gp, ldg, up, ldu, t, T, d, f, a, aligned, index = _ff_operands(x, w_gate, w_up, act, stream)
     dev = x.device
     dp, dt, lddh, _ = _matrices(dh, "dh", _FF_TYPES)
     L = lib()
@@ -987,10 +1000,10 @@ def gated_ff_backward(dh, x, w_gate, w_up, saved, act: str = "silu", want=(True,
     if not isinstance(saved, torch.Tensor) or saved.device != dev or not saved.is_contiguous() or \
             saved.dtype != torch.uint8 or saved.numel() != L.gspar_gated_ff_saved_bytes(T, f):
         raise ValueError("saved must be what a forward pass with save=True on these sizes kept")
-    dx = torch.empty((T, d), dtype=x.dtype, device=dev) if want[0] else None
-    dwg = torch.empty((f, d), dtype=x.dtype, device=dev) if want[1] else None
-    dwu = torch.empty((f, d), dtype=x.dtype, device=dev) if want[2] else None
-    _made_for(stream, dx, dwg, dwu)
+    dx = _empty((T, d), x.dtype, dev, stream) if want[0] else None
+    dwg = _empty((f, d), x.dtype, dev, stream) if want[1] else None
+    dwu = _empty((f, d), x.dtype, dev, stream) if want[2] else None
+    _lend(stream, dh, x, w_gate, w_up, saved)
     buf, nb, raw = _place(workspace, index, L.gspar_gated_ff_workspace_bytes(T, d, f, aligned, 1), stream)
     rc = L.gspar_gated_ff_backward(dp, lddh, xp, ldx, gp, ldg, up, ldu, saved.data_ptr(), t, T, d, f, a, _ptr(dx), d,
                                    _ptr(dwg), d, _ptr(dwu), d, buf, nb, raw)

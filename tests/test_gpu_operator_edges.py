@@ -269,3 +269,77 @@ def test_writes_are_seen_by_autograd(gs):
         t = torch.zeros((40, 64), device="cuda")
         gs.muon_step(t, torch.zeros_like(t), g, 0.1)
         assert bool(t.any())
+
+
+def test_results_made_for_another_stream(gs):
+    """A call on another stream gets no memory that the current one has yet to write: tensors given up there before
+    the call, with a long wait and a fill queued for them, leave the call's results alone; nor is what the call reads
+    or left behind handed out again before its stream is done with it."""
+    x, wg, wu, dh = ff_inputs(300, 128, 200, BF16, 70)
+    g = normal((300, 200), 74)
+    y = gs.gated_ff(x, wg, wu, save=True)
+    d = gs.gated_ff_backward(dh, x, wg, wu, y.saved)
+    o = gs.orthogonalize(g)
+    want = [t.clone() for t in (y.h, y.saved, d.dx, d.dw_gate, d.dw_up, o.o, o.flags)]
+    s = torch.cuda.Stream()
+    gs.gated_ff_backward(dh, x, wg, wu, gs.gated_ff(x, wg, wu, save=True, stream=s).saved, stream=s)  # its workspace
+    gs.orthogonalize(g, stream=s)
+    torch.cuda.synchronize()
+    shapes = [(t.shape, t.dtype) for t in want]
+    del y, d, o
+    s.wait_stream(torch.cuda.current_stream())
+    torch.cuda._sleep(200_000_000)
+    for _ in range(2):
+        old = [torch.empty(a, dtype=t, device="cuda") for a, t in shapes]
+        for t in old:
+            t.fill_(1)
+        del t, old
+    y = gs.gated_ff(x, wg, wu, save=True, stream=s)
+    d = gs.gated_ff_backward(dh, x, wg, wu, y.saved, stream=s)
+    o = gs.orthogonalize(g, stream=s)
+    got = (y.h, y.saved, d.dx, d.dw_gate, d.dw_up, o.o, o.flags)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    # inputs given up right after the call, while its stream still waits
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(200_000_000)
+    own = [t.clone() for t in (x, wg, wu, dh, g)]
+    s.wait_stream(torch.cuda.current_stream())
+    y = gs.gated_ff(*own[:3], save=True, stream=s)
+    d = gs.gated_ff_backward(own[3], *own[:3], y.saved, stream=s)
+    o = gs.orthogonalize(own[4], stream=s)
+    shapes = [(t.shape, t.dtype) for t in own]
+    del own
+    new = [torch.full(a, 1.0, dtype=t, device="cuda") for a, t in shapes]
+    torch.cuda.synchronize()
+    got = (y.h, y.saved, d.dx, d.dw_gate, d.dw_up, o.o, o.flags)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and all(bool((t == 1).all()) for t in new)
+
+
+def test_a_stream_of_another_device_is_refused(gs):
+    class Elsewhere:  # what is asked of a stream before anything is enqueued
+        device_index = torch.cuda.current_device() + 1
+
+    x, wg, wu, dh = ff_inputs(8, 16, 24, F16, 76)
+    saved = gs.gated_ff(x, wg, wu, save=True).saved
+    g = normal((8, 16), 78)
+    for call in (lambda s: gs.gated_ff(x, wg, wu, stream=s), lambda s: gs.gated_ff_backward(dh, x, wg, wu, saved, stream=s),
+                 lambda s: gs.orthogonalize(g, stream=s), lambda s: gs.muon_step(g, g.clone(), g.clone(), 0.1, stream=s)):
+        with pytest.raises(ValueError, match="stream"):
+            call(Elsewhere())
+
+
+def test_autograd_on_another_stream(gs):
+    """The block's backward pass goes to its forward pass's stream, and the gradients are the same."""
+    x, wg, wu, dh = ff_inputs(90, 64, 96, BF16, 79)
+    y = gs.gated_ff(x, wg, wu, save=True)
+    ref = gs.gated_ff_backward(dh, x, wg, wu, y.saved)
+    s = torch.cuda.Stream()
+    leaf = [t.clone().requires_grad_() for t in (x, wg, wu)]
+    s.wait_stream(torch.cuda.current_stream())
+    z = gs.gated_ff(*leaf, stream=s)
+    torch.cuda.current_stream().wait_stream(s)
+    z.h.backward(dh)
+    torch.cuda.synchronize()
+    assert torch.equal(z.h, y.h)
+    assert all(torch.equal(t.grad, r) for t, r in zip(leaf, (ref.dx, ref.dw_gate, ref.dw_up)))
