@@ -343,3 +343,19 @@ def test_autograd_on_another_stream(gs):
     torch.cuda.synchronize()
     assert torch.equal(z.h, y.h)
     assert all(torch.equal(t.grad, r) for t, r in zip(leaf, (ref.dx, ref.dw_gate, ref.dw_up)))
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("side", [1.0, -1.0])
+def test_slopes_of_the_largest_sums(gs, act, side):
+    """Sums as large as bfloat16's products make them: the slope is one, or zero on the other side."""
+    for k in (1e10, 1e17, 1e18, 1.5e19):  # act's argument is +-k^2, the up projection one, dh 1 / k
+        x = torch.full((1, 1), k, dtype=BF16, device="cuda")
+        wg, wu = torch.full_like(x, side * k), 1 / x
+        dh = 1 / x
+        y = gs.gated_ff(x, wg, wu, act, save=True)
+        d = gs.gated_ff_backward(dh, x, wg, wu, y.saved, act)
+        # dx = dh u act'(g) wg + dh act(g) wu: 1 + 1 or 0; rounded to 8 bits some six times on the way
+        on = 1.0 if side > 0 else 0.0
+        assert abs(float(d.dx) - 2 * on) <= 0.05, (k, float(d.dx))
+        assert abs(float(d.dw_gate) - on) <= 0.05 and bool(torch.isfinite(d.dw_up).all())
