@@ -815,6 +815,13 @@ def _place(workspace, index, nbytes, stream):
     return buf.data_ptr(), nb, raw
 
 
+def _coefficients(c):
+    c = tuple(c)
+    if len(c) != 3:
+        raise ValueError(f"a step has three coefficients, not {len(c)}")
+    return (ctypes.c_double * 3)(*c)
+
+
 @dataclass
 class Orthogonal:
     """o: the orthogonalised matrices; flags: int32, one per matrix."""
@@ -861,7 +868,7 @@ def orthogonalize(g, steps: int = 5, coefficients=NS_COEFFICIENTS, eps: float = 
     _lend(stream, g, out)
     L = lib()
     buf, nb, raw = _place(workspace, dev, L.gspar_orthogonalize_workspace_bytes(batch, m, n, ot), stream)
-    c = (ctypes.c_double * 3)(*coefficients)
+    c = _coefficients(coefficients)
     rc = L.gspar_orthogonalize(gp, gt, batch, m, n, ldg, sg, int(steps), c, float(eps), float(scale), op, ot, ldo, so,
                                fl.data_ptr(), buf, nb, raw)
     _check(rc, "gspar_orthogonalize")
@@ -888,7 +895,7 @@ def muon_step(w, momentum, grad, lr: float, beta: float = 0.95, nesterov: bool =
     _lend(stream, w, momentum, grad, w_copy)
     L = lib()
     buf, nb, raw = _place(workspace, dev, L.gspar_orthogonalize_workspace_bytes(batch, m, n, wt), stream)
-    c = (ctypes.c_double * 3)(*coefficients)
+    c = _coefficients(coefficients)
     rc = L.gspar_muon_step(wp, wt, ldw, sw, mp, mt, ldm, sm, gp, gt, ldg, sg, batch, m, n, float(lr), float(beta),
                            1 if nesterov else 0, float(weight_decay), float(scale), int(steps), c, float(eps), cp, ct, ldc, sc,
                            fl.data_ptr(), buf, nb, raw)

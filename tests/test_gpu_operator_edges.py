@@ -359,3 +359,12 @@ def test_slopes_of_the_largest_sums(gs, act, side):
         on = 1.0 if side > 0 else 0.0
         assert abs(float(d.dx) - 2 * on) <= 0.05, (k, float(d.dx))
         assert abs(float(d.dw_gate) - on) <= 0.05 and bool(torch.isfinite(d.dw_up).all())
+
+
+def test_coefficients_are_three(gs):
+    g = normal((8, 8), 80)
+    for bad in ((1.5, -0.5), (1.5, -0.5, 0.0, 0.0), ()):
+        with pytest.raises(ValueError):
+            gs.orthogonalize(g, coefficients=bad)
+        with pytest.raises(ValueError):
+            gs.muon_step(g, g.clone(), g.clone(), 0.1, coefficients=bad)
