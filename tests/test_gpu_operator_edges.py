@@ -368,3 +368,69 @@ def test_coefficients_are_three(gs):
             gs.orthogonalize(g, coefficients=bad)
         with pytest.raises(ValueError):
             gs.muon_step(g, g.clone(), g.clone(), 0.1, coefficients=bad)
+
+
+@pytest.mark.parametrize("shape", [(3, 40, 33), (5, 64, 130), (17, 100, 64), (2, 300, 520), (33, 128, 192)], ids=str)
+def test_a_batch_against_calls_of_its_own(gs, shape):
+    """A matrix of a batch and the same matrix alone may go by different tiles: both are within the tolerance of the
+    64-bit steps, so within twice that of each other."""
+    for dtype, most in ((F32, 2e-5), (BF16, 5e-3)):
+        g = normal(shape, 90, dtype)
+        o = gs.orthogonalize(g).o
+        w, mom = normal(shape, 91, dtype), normal(shape, 92)
+        alone = [(a.clone(), b.clone()) for a, b in zip(w, mom)]
+        gs.muon_step(w, mom, g, 0.1)
+        for k in range(shape[0]):
+            assert off(o[k], gs.orthogonalize(g[k]).o) <= 2 * most
+            gs.muon_step(*alone[k], g[k], 0.1)
+            # momentum: the same operations; weights: a tenth of the result, or their own rounding
+            assert torch.equal(mom[k], alone[k][1]) and off(w[k], alone[k][0]) <= 2 * most
+
+
+def test_backward_offsets_past_32_bits(gs):
+    """Gradients of the sums and kept sums past 2^32 bytes: dx of the first, middle and last tokens, and the weights'
+    gradients of the first, middle and last units over all tokens."""
+    T, d, f = 140_003, 64, 16_392
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+
+    def t(*s, k=1.0):
+        return (k * torch.randn(s, generator=gen, device="cuda")).to(BF16)
+
+    x, wg, wu, dh = t(T, d), t(f, d, k=0.125), t(f, d, k=0.125), torch.empty((T, f), dtype=BF16, device="cuda")
+    for r in range(0, T, 10_000):
+        dh[r:r + 10_000] = t(min(10_000, T - r), f, k=0.1)
+    y = gs.gated_ff(x, wg, wu, save=True)
+    got = gs.gated_ff_backward(dh, x, wg, wu, y.saved)
+
+    def sums(tokens, units):
+        a, b, c, e = (v.detach().cpu().double() for v in (x[tokens], wg[units], wu[units], dh[tokens][:, units]))
+        g, u = a @ b.t(), a @ c.t()
+        s = torch.sigmoid(g)
+        return e * u * s * (1 + g * (1 - s)), e * g * s, a, b, c
+
+    # 2-norms: one rounding of each factor and one of the result, 2 u
+    for rows in (slice(0, 5), slice(131_000, 131_005), slice(T - 5, T)):
+        dg, du, _, b, c = sums(rows, slice(None))
+        assert off(got.dx[rows], dg @ b + du @ c) <= 2.0 ** -7
+    for units in (slice(0, 5), slice(8_190, 8_195), slice(f - 5, f)):
+        dg, du, a, _, _ = sums(slice(None), units)
+        assert off(got.dw_gate[units], dg.t() @ a) <= 2.0 ** -7 and off(got.dw_up[units], du.t() @ a) <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("shape", [(1100, 1000, 1024), (33_000, 128, 264), (33_000, 127, 261)], ids=str)
+def test_update_offsets_past_32_bits(gs, shape):
+    """Batches of more than 2^32 bytes: the first, a middle and the last matrix against the same ones alone."""
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    g = torch.empty(shape, device="cuda")
+    for k in range(0, shape[0], 1000):
+        g[k:k + 1000].normal_(generator=gen)
+    out = gs.orthogonalize(g)
+    assert not out.flags.any()
+    for k in (0, shape[0] // 2, shape[0] - 1):
+        assert off(out.o[k], gs.orthogonalize(g[k]).o) <= 4e-5
+    w, mom = torch.zeros_like(g), torch.zeros_like(g)
+    assert not gs.muon_step(w, mom, g, 1.0).any()
+    for k in (0, shape[0] // 2, shape[0] - 1):
+        assert torch.equal(mom[k], g[k]) and off(w[k], -out.o[k]) <= 4e-5
