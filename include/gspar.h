@@ -330,7 +330,7 @@ int gspar_gated_ff_forward(const void* x, int64_t ldx, const void* w_gate, int64
 /* The block's gradients from dh [tokens][d_hidden] and the forward pass's x, weights and saved buffer:
  * dx [tokens][d_in], dw_gate and dw_up [d_hidden][d_in], each NULL where it is not wanted, all of
  * `type`. The gradients of act's argument and of the up projection are rounded to `type` once, for the
- * products; their sums are in 32 bits. No token gives zero gradients of the weights.
+ * products, whose sums are in 32 bits: a result's error is about sqrt(2) times its own rounding's. No token gives zero gradients of the weights.
  * Errors: as above, and GSPAR_ERR_ARG for a NULL saved. */
 int gspar_gated_ff_backward(const void* dh, int64_t lddh, const void* x, int64_t ldx, const void* w_gate, int64_t ldg,
                             const void* w_up, int64_t ldu, const void* saved, int type, int64_t tokens, int64_t d_in,

@@ -13,9 +13,9 @@
 // A block of 16 columns of results takes, of 16 G neighbouring columns, a four of each 4 G: a lane then ends with
 // 4 G neighbouring results of a row and stores them at once (G blocks of four; G = 4, or 2 for narrow tiles).
 //
-// What bounds it: the matrix cores and the power they may draw. 256 x 256 results by 8 waves: 8192 x 4096 x 8192
-// in bfloat16 takes 378 us (1455 TFLOP/s) along K, 393 with one side down it and 436 with both, where the installed
-// library's product of 8192^3 reaches 1420 TFLOP/s; 4096^3 in pairs takes 251 us, 1640 TFLOP/s of products. Small
+// What bounds it: the matrix cores and the power they may draw. The three products of 8192 x 4096 x 12288 in bfloat16 by
+// tiles of 256 x 256, traced: 1,218 TFLOP/s with both sides along K (and the feed-forward's epilogue), 1,313 with one
+// down it, 1,109 with both, where the installed library's product of 8192^3 reaches 1,420. Small
 // products take small tiles, for there they have too few to fill 256 compute units, and are bound by the latency of
 // a slice.
 #ifndef GSPAR_DENSE_H
@@ -637,13 +637,20 @@ struct Way {
 };
 
 // The way that takes least time: rounds of workgroups times the slices of each and the time of a slice, and the time
-// that a round's first fetches and its results take, `tiles(side)` being the number of tiles of that side, plus the second launch and the parts' bytes. Measured in us a
-// slice, 16-bit numbers and pairs of them: 256 x 256: 1.5 and 1.97 (4096^3 in 100 and 251 us); 192 x 192: 0.95 and
-// 1.2; 128 x 128, two on a compute unit: 1.0 and 1.16; 128 x 128 by two groups of waves, one on a compute unit: 0.6;
-// 64 x 64 by two groups: 0.26 (1024 x 512 x 4608 in 43 us by 128 x 128 and in 17 to 21 by 64 x 64, which has 128 tiles
-// where the other has 32), and by one, two on a compute unit: 0.5 (512 tiles of 1000 in pairs at once in 21.7 us and in
-// two rounds of 256 by two groups in 23.8; 136 tiles of 2048 in 23.3 and 17.6; not for parts of K: 128 tiles of 5632 in
-// four take 17.2 us and by two groups 15.8). Parts, 5 us and their bytes at 8 TB/s (they stay in the caches): the
+// that a round's first fetches and its results take, `tiles(side)` being the number of tiles of that side, plus the
+// second launch and the parts' bytes. us a slice, 16-bit numbers (a slice is 64 of K) and pairs of them (32 of K): the
+// figures that choose best among the products of whole calls, and in brackets what one round of full tiles takes, 16
+// slices and 64 (along K and with one side down it). Small tiles take as long for either, for they are bound by a slice's
+// bytes on their way into LDS, which are the same:
+//   256 x 256                                       1.5 and 1.97  [1.5 to 1.85 and 1.95]
+//   192 x 192                                       0.95 and 1.2  [0.92 and 1.14]
+//   128 x 128, two on a compute unit                1.0 and 1.16  [0.88 to 0.91 and 1.10]
+//   128 x 128 by two groups of waves, one on a unit 0.6 for both  [0.50 to 0.53 and 0.55 to 0.57]
+//   64 x 64 by two groups                           0.26 for both [0.21 and 0.20 to 0.22]
+//   64 x 64 by one, two on a compute unit           0.5 for both  [0.36 to 0.43 and 0.37 to 0.45]
+// 1024 x 512 x 4608 takes 43 us by 128 x 128 and 17 to 21 by 64 x 64, which has 128 tiles where the other has 32; 512
+// tiles of 64 x 64 of 1000 in pairs at once 21.7 us and in two rounds of 256 by two groups 23.8; 136 tiles of 2048 in pairs
+// 23.3 and 17.6; not for parts of K: 128 tiles of 5632 in four take 17.2 us and by two groups 15.8. Parts, 5 us and their bytes at 8 TB/s (they stay in the caches): the
 // 512 x 512 of a 512 x 4608 matrix in pairs takes 32 us whole and 16.5 in parts. The rounds' ends count where K is
 // short: six products 1024 x 4096 x 1024 take 94 us by 256 x 256 (two rounds of 16 slices) and 88 by 128 x 128.
 template <class Tiles>

@@ -7,7 +7,8 @@
 //
 // Backward: dG = dh u act'(g) and dU = dh act(g) from the kept sums in one pass, then
 // dx = [dG dU] [Wg; Wu] and [dWg; dWu] = [dG dU]^T x as one product each. dG and dU are rounded to the
-// tensors' type once: a product of matrix cores takes 16-bit factors; its sums are of 32 bits.
+// tensors' type once: a product of matrix cores takes 16-bit factors; its sums are of 32 bits. A gradient's error (2-norm)
+// so is sqrt(2) times its own rounding: 2.35e-3 for bfloat16, whose rounding makes 1.66e-3.
 #include "dense.h"
 
 #include <algorithm>
@@ -76,9 +77,9 @@ struct FF {
   Saved kept;
 };
 
-// Bound by the matrix cores where tokens are many: 8192 x 4096 x 12288 in bfloat16 in 1,344 us (1,227 TFLOP/s) with the
-// sums kept (604 MB of its writes) and 1,198 without; 1003 x 2048 x 5461 in float16 in 53 (172 tiles of 256 x 256 on 256
-// compute units).
+// Bound by the matrix cores where tokens are many: 8192 x 4096 x 12288 in bfloat16 in 1,354 us (1,218 TFLOP/s, traced) with
+// the sums kept (604 MB of its writes) and 1,198 without; 1003 x 2048 x 5461 in float16 in 52, a call (172 tiles of
+// 256 x 256 on 256 compute units).
 template <class T, class C, bool kKeep, int kAct>
 __global__ void __launch_bounds__(C::kThreads, C::kThreads / 256) k_ff_forward(FF J, int tm, int tn) {
   int ti, tj;
@@ -129,8 +130,9 @@ __global__ void __launch_bounds__(C::kThreads, C::kThreads / 256) k_ff_forward(F
 // 16 UB units of both projections and up to 16 TT tokens; its eight waves share out D, and add their sums in LDS.
 // The products are D[unit][token] with the weights' rows on the left. A lane reads 8 elements of a row at once, at any
 // alignment that the type allows, so no operand is copied; rows past F or T repeat the last one (a row of results
-// depends on its own operand's row alone) and are not stored. 24 x 4096 x 12288: 41 us, 4.9 TB/s; one token of
-// 1024 x 2816: 4.9 us, latency. (By tiles, the weights through LDS: 56 and 16 us a call; so 47 and 9.)
+// depends on its own operand's row alone) and are not stored. 24 x 4096 x 12288: 48 us, 4.2 TB/s (41 where a
+// cache still holds some of the last call's weights); one token of 1024 x 2816: 5.2 us, latency. (By tiles, the weights
+// through LDS: 56 and 16 us a call; so 47 and 10.)
 struct Few {
   const uint16_t *x, *wg, *wu;
   int64_t ldx, ldg, ldu;
@@ -289,7 +291,7 @@ __global__ void __launch_bounds__(256) k_pack(Copies J, int per_row) {
 }
 
 // dG and dU, [tokens][2 ld]: dG in the first ld columns and dU in the others, zeros past F. Eight of each a
-// thread. Bound by its bytes: 8192 x 12288 in bfloat16 (1.2 GB) in 257 us, 4.7 TB/s.
+// thread. Bound by its bytes: 8192 x 12288 in bfloat16 (1.2 GB) in 260 us, 4.6 TB/s.
 template <class T, int kAct>
 __global__ void __launch_bounds__(256) k_ff_between(FF J, const uint16_t* dh, int64_t lddh, uint16_t* dgu, int64_t ld) {
   const int64_t f = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
@@ -321,7 +323,7 @@ __global__ void __launch_bounds__(256) k_ff_between(FF J, const uint16_t* dh, in
 // dx = [dG dU] [Wg; Wu] (kDown = false), or [dWg; dWu] = [dG dU]^T x (kDown): out[i][j] = sum_k A(i, k) B(j, k),
 // A along K or down it, B down K. Rows of results in [cut0, cut1) are not there (the padding between dG and
 // dU); those from cut1 on go to out1. Bound by the matrix cores where all sides are long: 8192 x 4096 x 12288 in
-// bfloat16, dx 1,262 us (1,307 TFLOP/s), dW, both operands of which lie down K, 1,500 (1,099).
+// bfloat16, dx 1,257 us (1,313 TFLOP/s), dW, both operands of which lie down K, 1,487 (1,109).
 struct Product {
   Rows a, b0, b1;
   int steps, cut;  // slices of K; those of b0
