@@ -760,7 +760,8 @@ def _matrices(t, what, types, like=None):
     if nd == 3 and shape[0] > 1:
         stride = st[0]
         if stride < (m - 1) * ld + n:
-            raise ValueError(f"{what} must not repeat its elements (an expanded tensor has to be made contiguous)")
+            raise ValueError(f"{what}'s matrices must lie one behind the other (an expanded or interleaved batch has to be "
+                             "made contiguous)")
     if ld < n:
         raise ValueError(f"{what} must not repeat its elements (an expanded tensor has to be made contiguous)")
     return t.data_ptr(), _TYPE[t.dtype], ld, stride

@@ -434,3 +434,19 @@ def test_update_offsets_past_32_bits(gs, shape):
     assert not gs.muon_step(w, mom, g, 1.0).any()
     for k in (0, shape[0] // 2, shape[0] - 1):
         assert torch.equal(mom[k], g[k]) and off(w[k], -out.o[k]) <= 4e-5
+
+
+def test_autograd_without_tokens(gs):
+    x, wg, wu, _ = ff_inputs(0, 64, 80, BF16, 100)
+    leaf = [t.clone().requires_grad_() for t in (x, wg, wu)]
+    gs.gated_ff(*leaf).h.sum().backward()
+    assert leaf[0].grad.shape == (0, 64) and not leaf[1].grad.any() and not leaf[2].grad.any()
+
+
+def test_refusals_name_the_batch(gs):
+    """Heads that lie side by side in a row are no batch that the operators take, nor is one matrix repeated."""
+    g = normal((40, 3, 16), 101)
+    for bad in (g.permute(1, 0, 2), g[:, 0].expand(3, 40, 16)):
+        with pytest.raises(ValueError, match="one behind the other"):
+            gs.orthogonalize(bad)
+    assert not gs.orthogonalize(g.permute(1, 0, 2).contiguous()).flags.any()
